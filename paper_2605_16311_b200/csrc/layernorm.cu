@@ -896,21 +896,23 @@ __global__ void __launch_bounds__(WIDE_THREADS) dx_wide_kernel(const Backward a)
   }
 }
 
-// rows: of a thread block at a time.  shared: dynamic shared memory (0: a kernel that loads its rows directly).
+// rows: of a thread block at a time.  shared: dynamic shared memory (0: a kernel that loads its rows directly); limit: the most
+// that any call asks of this kernel.  The limit that the runtime keeps belongs to the kernel and the device, whichever context
+// sets it: it is always set to `limit`, so that no call takes away what another one needs.
 struct Choice {
   void* fn;
   int threads, rows;
-  size_t shared;
+  size_t shared, limit;
   bool wide;
 };
 template <typename AT, int T, int E, bool VEC>
-Choice forward_choice() { return {(void*)forward_kernel<AT, T, E, VEC>, Group<T>::THREADS, Group<T>::ROWS, 0, false}; }
+Choice forward_choice() { return {(void*)forward_kernel<AT, T, E, VEC>, Group<T>::THREADS, Group<T>::ROWS, 0, 0, false}; }
 template <typename AT, int T, int E>
 Choice forward_ring(int arrays) {
   using One = ForwardRing<AT, T, E, 1>;
   using Two = ForwardRing<AT, T, E, 2>;
-  if (arrays == 1) return {(void*)forward_ring_kernel<AT, T, E, 1>, One::NT, One::GROUPS, One::BYTES, false};
-  return {(void*)forward_ring_kernel<AT, T, E, 2>, Two::NT, Two::GROUPS, Two::BYTES, false};
+  if (arrays == 1) return {(void*)forward_ring_kernel<AT, T, E, 1>, One::NT, One::GROUPS, One::BYTES, One::BYTES, false};
+  return {(void*)forward_ring_kernel<AT, T, E, 2>, Two::NT, Two::GROUPS, Two::BYTES, Two::BYTES, false};
 }
 
 template <typename AT, bool VEC>
@@ -932,7 +934,7 @@ Choice choose_forward(int64_t cols) {
     if (cols <= 1024 * 8) return forward_choice<AT, 1024, 8, VEC>();
     if (cols <= 1024 * 12) return forward_choice<AT, 1024, 12, VEC>();
     if (cols <= 1024 * 16) return forward_choice<AT, 1024, 16, VEC>();
-    return {(void*)forward_wide_kernel<AT, 1>, WIDE_THREADS, 1, 0, true};
+    return {(void*)forward_wide_kernel<AT, 1>, WIDE_THREADS, 1, 0, 0, true};
   } else {
     if (cols <= 32 * 16) return forward_choice<AT, 32, 16, true>();
     if (cols <= 32 * 24) return forward_choice<AT, 32, 24, true>();
@@ -941,7 +943,7 @@ Choice choose_forward(int64_t cols) {
     if (cols <= 256 * 16) return forward_choice<AT, 256, 16, true>();
     if (cols <= 512 * 16) return forward_choice<AT, 512, 16, true>();
     if (cols <= 1024 * 16) return forward_choice<AT, 1024, 16, true>();
-    return {(void*)forward_wide_kernel<AT, Unit<AT>::N>, WIDE_THREADS, 1, 0, true};
+    return {(void*)forward_wide_kernel<AT, Unit<AT>::N>, WIDE_THREADS, 1, 0, 0, true};
   }
 }
 // (aligned rows of 129 .. 8192 entries)
@@ -957,11 +959,11 @@ Choice choose_forward_ring(int64_t cols, int arrays) {
 }
 
 template <typename AT, int T, int E, bool VEC>
-Choice backward_choice() { return {(void*)backward_kernel<AT, T, E, VEC>, BackGroup<T>::THREADS, BackGroup<T>::ROWS, 0, false}; }
+Choice backward_choice() { return {(void*)backward_kernel<AT, T, E, VEC>, BackGroup<T>::THREADS, BackGroup<T>::ROWS, 0, 0, false}; }
 template <typename AT, int T, int E>
 Choice backward_ring(int arrays) {
   using R = BackwardRing<AT, T, E>;
-  return {(void*)backward_ring_kernel<AT, T, E>, R::NT, R::GROUPS, R::bytes(arrays), false};
+  return {(void*)backward_ring_kernel<AT, T, E>, R::NT, R::GROUPS, R::bytes(arrays), R::bytes(3), false};
 }
 
 template <typename AT, bool VEC>
@@ -969,8 +971,8 @@ Choice choose_backward(int64_t cols, int arrays) {
   if (cols <= 4 * 8) return backward_choice<AT, 4, 8, VEC>();
   if (cols <= 8 * 8) return backward_choice<AT, 8, 8, VEC>();
   if (cols <= 16 * 8) return backward_choice<AT, 16, 8, VEC>();
-  if (cols > 1024 * 16) return {(void*)dx_wide_kernel<AT, VEC ? Unit<AT>::N : 1>, WIDE_THREADS, 1, 0, true};
-  if (cols > 512 * 16) return {(void*)dx_kernel<AT, 1024, 16, VEC>, 1024, 1, 0, true};
+  if (cols > 1024 * 16) return {(void*)dx_wide_kernel<AT, VEC ? Unit<AT>::N : 1>, WIDE_THREADS, 1, 0, 0, true};
+  if (cols > 512 * 16) return {(void*)dx_kernel<AT, 1024, 16, VEC>, 1024, 1, 0, 0, true};
   if constexpr (VEC) {
     if (cols <= 32 * 8) return backward_ring<AT, 32, 8>(arrays);
     if (cols <= 32 * 16) return backward_ring<AT, 32, 16>(arrays);
@@ -1018,7 +1020,7 @@ struct signmuon_layernorm {
     for (int i = 0; i < std::min(n_fits, 8); ++i)
       if (fits[i].fn == k.fn && fits[i].shared == k.shared) return fits[i].blocks;
     int blocks = 0;
-    if ((k.shared && cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.shared) != cudaSuccess) ||
+    if ((k.shared && cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.limit) != cudaSuccess) ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, k.fn, k.threads, k.shared) != cudaSuccess || blocks < 1)
       return 0;
     fits[n_fits++ % 8] = {k.fn, k.shared, blocks};
