@@ -1050,7 +1050,9 @@ int signmuon_adamw_bind(signmuon_adamw* c, void* dev_state, size_t state_bytes, 
   const bool small = c->params.size() <= SMALL;
   void* step = small ? step_kernel<SMALL>(c) : step_kernel<LARGE>(c);
   void* norm = small ? (void*)grad_norm_kernel<SMALL> : (void*)grad_norm_kernel<LARGE>;
-  if ((c->shared && cudaFuncSetAttribute(step, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)c->shared) != cudaSuccess) ||
+  // The limit of dynamic shared memory belongs to the kernel and the device, not to this context: always the most that any
+  // context asks of it, so that none lowers it under another.
+  if ((c->shared && cudaFuncSetAttribute(step, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RING_LIMIT) != cudaSuccess) ||
       cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ_step, step, THREADS, c->shared) != cudaSuccess ||
       cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ_norm, norm, THREADS, 0) != cudaSuccess) {
     cudaGetLastError();
