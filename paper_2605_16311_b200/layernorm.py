@@ -157,7 +157,8 @@ class LayerNorm:
 
     def apply(self, x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None):
         """y, or (y, x + residual), for torch's autograd.  gamma and beta are [cols] (their gradient is then the sum over
-        the workers) or [num_workers, cols] views expanded from one row, which receive every worker's own."""
+        the workers) or [num_workers, cols] views expanded from one row, which receive every worker's own.  There are no
+        second derivatives: asking for one raises."""
         y, s = _Function.apply(self, x, gamma, beta, residual)
         return y if residual is None else (y, s)
 
@@ -170,7 +171,7 @@ class _Function(torch.autograd.Function):
                 raise ValueError(f"{name} is not [{ln.cols}], nor [{ln.num_workers}, {ln.cols}] expanded from one row")
         one = [w[0] if w is not None and w.dim() == 2 else w for w in (gamma, beta)]
         y, mean, rstd, s = ln.forward(x, *one, residual=residual)
-        fn.save_for_backward(s, one[0], mean, rstd)
+        fn.save_for_backward(s, gamma, mean, rstd)
         fn.ln, fn.apart, fn.has = ln, [w is not None and w.dim() == 2 for w in (gamma, beta)], (beta is not None, residual is not None)
         if residual is None:
             fn.mark_non_differentiable(total := s.new_empty(0))
@@ -179,10 +180,30 @@ class _Function(torch.autograd.Function):
 
     @staticmethod
     def backward(fn, dy, ds):
-        s, gamma, mean, rstd = fn.saved_tensors
         bias, residual = fn.has
-        dx, dgamma, dbeta = fn.ln.backward(dy.contiguous(), s, gamma, mean, rstd, dsum=ds.contiguous() if residual else None, bias=bias)
-        dgamma = dgamma if fn.apart[0] else dgamma.float().sum(0).to(dgamma.dtype)
-        if bias and not fn.apart[1]:
-            dbeta = dbeta.float().sum(0).to(dbeta.dtype)
+        # (with create_graph as a function of its inputs, so that whoever differentiates it meets the refusal)
+        call = _Backward.apply if torch.is_grad_enabled() else _gradients
+        dx, dgamma, dbeta = call(fn.ln, fn.apart, bias, dy, ds if residual else None, *fn.saved_tensors)
         return None, dx, dgamma, dbeta, dx if residual else None
+
+
+def _gradients(ln, apart, bias, dy, ds, s, gamma, mean, rstd):
+    dx, dgamma, dbeta = ln.backward(dy.contiguous(), s, gamma[0] if apart[0] else gamma, mean, rstd,
+                                    dsum=None if ds is None else ds.contiguous(), bias=bias)
+    dgamma = dgamma if apart[0] else dgamma.float().sum(0).to(dgamma.dtype)
+    if bias and not apart[1]:
+        dbeta = dbeta.float().sum(0).to(dbeta.dtype)
+    return dx, dgamma, dbeta
+
+
+class _Backward(torch.autograd.Function):
+    """The backward pass under create_graph.  once_differentiable would not do: its error hangs on a node of its own, which
+    autograd.grad leaves out where the inputs asked for are reached on other ways."""
+
+    @staticmethod
+    def forward(fn, *args):
+        return _gradients(*args)
+
+    @staticmethod
+    def backward(fn, *grads):
+        raise RuntimeError("layer norm has no second derivatives")
