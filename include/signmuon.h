@@ -475,9 +475,10 @@ void signmuon_adamw_destroy(signmuon_adamw* ctx);
  *             dgamma_k = sum of dy xhat, dbeta_k = sum of dy over worker k's rows
  *
  * Statistics and sums are float32, every result is rounded once, and every sum has an order that the sizes
- * and the alignment fix: the same call gives the same bits.  Rows may lie apart (ld_*), entries of a row are neighbours.  Nothing is required of alignment beyond
- * an entry's own; 16-byte aligned pointers and row distances are faster.
- * One context must not run two backward passes at once on different streams (they share the workspace). */
+ * and the alignment fix: the same call gives the same bits.  Rows may lie apart (ld_*), entries of a row are neighbours.
+ * Nothing is required of alignment beyond an entry's own; 16-byte aligned pointers and row distances are faster.
+ * Several threads may use one bound context at once, but its backward passes share the workspace: one is called after the
+ * other has returned, and on the same stream or ordered behind it. */
 typedef struct signmuon_layernorm signmuon_layernorm;   /* opaque host object */
 
 typedef struct {

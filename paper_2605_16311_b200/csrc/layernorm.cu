@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <new>
 
@@ -1010,20 +1011,20 @@ struct signmuon_layernorm {
   float* workspace = nullptr;
   bool bound = false;
   int sms = 0;
-  int sticky = SIGNMUON_OK;
-  struct Fit { void* fn; size_t shared; int blocks; };
-  Fit fits[8] = {};              // thread blocks of a kernel that an SM holds, asked of the runtime once
-  int n_fits = 0;
+  std::atomic<int> sticky{SIGNMUON_OK};
+  // Thread blocks of a kernel that an SM holds, asked of the runtime once for each kind of call; 0: not yet.  Threads that ask
+  // at once get the same answer.
+  enum Kind { FORWARD, FORWARD_RESIDUAL, BACKWARD, BACKWARD_DSUM, BACKWARD_SINGLE, KINDS };
+  std::atomic<int> fits[KINDS] = {};
 
   // Also allows the kernel its dynamic shared memory.  0: the runtime refused.
-  int resident(const Choice& k) {
-    for (int i = 0; i < std::min(n_fits, 8); ++i)
-      if (fits[i].fn == k.fn && fits[i].shared == k.shared) return fits[i].blocks;
-    int blocks = 0;
-    if ((k.shared && cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.limit) != cudaSuccess) ||
+  int resident(const Choice& k, int kind) {
+    int blocks = fits[kind].load(std::memory_order_acquire);
+    if (blocks) return blocks;
+    if ((k.limit && cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.limit) != cudaSuccess) ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, k.fn, k.threads, k.shared) != cudaSuccess || blocks < 1)
       return 0;
-    fits[n_fits++ % 8] = {k.fn, k.shared, blocks};
+    fits[kind].store(blocks, std::memory_order_release);
     return blocks;
   }
 };
@@ -1066,7 +1067,7 @@ int signmuon_layernorm_bind(signmuon_layernorm* c, void* dev_workspace, size_t w
   }
   if (major != 10) return SIGNMUON_ERR_UNSUPPORTED_ARCH;
   c->sms = sms;
-  c->n_fits = 0;
+  for (auto& f : c->fits) f = 0;
   c->workspace = static_cast<float*>(dev_workspace);
   c->bound = true;
   c->sticky = SIGNMUON_OK;
@@ -1110,7 +1111,7 @@ int signmuon_layernorm_forward(signmuon_layernorm* c, const signmuon_layernorm_f
   if (vec && cols > 16 * 8 && cols <= 512 * 16) {
     const int arrays = q.residual ? 2 : 1;
     const Choice ring = half ? choose_forward_ring<bf16>(cols, arrays) : choose_forward_ring<float>(cols, arrays);
-    const int64_t blocks = (int64_t)c->resident(ring) * c->sms;
+    const int64_t blocks = (int64_t)c->resident(ring, arrays == 2 ? c->FORWARD_RESIDUAL : c->FORWARD) * c->sms;
     if (blocks == 0) e = cudaErrorUnknown;
     else if (q.rows > 2 * blocks * ring.rows) {       // every group meets three rows or more: fetching ahead pays
       f = ring;
@@ -1170,7 +1171,7 @@ int signmuon_layernorm_backward(signmuon_layernorm* c, const signmuon_layernorm_
   const bool weights = q.dgamma || q.dbeta;
   // one wave of thread blocks, every group with a row at least; the columns' kernel shares a row out over several
   const int64_t across = COLUMN_THREADS * (vec ? unit : 1), side = (cols + across - 1) / across;
-  const int blocks = f.wide ? 8 : c->resident(f);
+  const int blocks = f.wide ? 8 : c->resident(f, !vec ? c->BACKWARD_SINGLE : q.dsum ? c->BACKWARD_DSUM : c->BACKWARD);
   const int64_t target = std::min<int64_t>(c->max_parts, f.wide ? (c->sms * 8 + side - 1) / side : (int64_t)c->sms * blocks);
   // rows of a part: the columns' kernel writes two floats for each that it sums; up to three rows a group stay with one thread
   // block, since two more rows cost it less than the launch of the joining kernel

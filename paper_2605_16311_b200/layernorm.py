@@ -5,11 +5,13 @@
     dx, dgamma, dbeta = ln.backward(dy, s, gamma, mean, rstd, dsum=ds) # dgamma, dbeta: [num_workers][cols]
 
 One object serves every layer norm of a width; `apply` joins the two passes for torch's autograd.  The rows of x are
-num_workers equal runs, worker after worker.
+num_workers equal runs, worker after worker.  Threads may use one object at once, but its backward passes share the
+workspace: one is called after the other has returned, and on the same stream or ordered behind it.
 """
 from __future__ import annotations
 
 import ctypes as C
+import threading
 from typing import Optional
 
 import torch
@@ -18,6 +20,14 @@ from . import binding as B
 
 _TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
 _stream = torch._C._cuda_getCurrentRawStream     # (a torch.cuda.Stream object costs 2 us)
+
+
+class _Arguments(threading.local):
+    """What a call fills in, for each thread its own: the library is called without the interpreter's lock."""
+
+    def __init__(self, one: torch.Tensor):
+        self.forward, self.backward = B.LayerNormForwardStruct(), B.LayerNormBackwardStruct()
+        self.statistics = one
 
 
 class LayerNorm:
@@ -40,8 +50,8 @@ class LayerNorm:
                      "signmuon_layernorm_bind")
         # patterns to allocate by, of one entry each: empty_like costs less than half of empty
         self._weight_gradient = torch.empty(1, dtype=self.grad_dtype, device=self.device).expand(num_workers, cols)
-        self._one = self._statistics = torch.empty(1, dtype=torch.float32, device=self.device)
-        self._forward_args, self._backward_args = B.LayerNormForwardStruct(), B.LayerNormBackwardStruct()
+        self._one = torch.empty(1, dtype=torch.float32, device=self.device)
+        self._mine = _Arguments(self._one)
 
     def close(self):
         if self.ctx:
@@ -88,7 +98,8 @@ class LayerNorm:
                 residual: Optional[torch.Tensor] = None, stats: bool = True, out: Optional[torch.Tensor] = None):
         """(y, mean, rstd, s).  s is x + residual, or x itself without one; mean and rstd are None without `stats`.
         gamma None: ones, beta None: zeros.  `out` takes y, and may be x."""
-        a = self._forward_args
+        mine = self._mine
+        a = mine.forward
         a.ld_x = self._rows(x, "x")
         rows = a.rows = x.numel() // self.cols
         y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
@@ -103,9 +114,9 @@ class LayerNorm:
             a.ld_sum, a.sum = self.cols, s.data_ptr()
         mean = rstd = None
         if stats:
-            if self._statistics.numel() != rows:
-                self._statistics = self._one.expand(rows)
-            mean, rstd = torch.empty_like(self._statistics), torch.empty_like(self._statistics)
+            if mine.statistics.numel() != rows:
+                mine.statistics = self._one.expand(rows)
+            mean, rstd = torch.empty_like(mine.statistics), torch.empty_like(mine.statistics)
             a.mean, a.rstd = mean.data_ptr(), rstd.data_ptr()
         else:
             a.mean = a.rstd = None
@@ -121,7 +132,7 @@ class LayerNorm:
         """(dx, dgamma, dbeta) with dgamma, dbeta [num_workers][cols], dbeta None without `bias`.  s, mean and rstd are those
         of the forward pass; dsum is the gradient that reaches s on another way and is added to dx.  `out` takes dx, and may
         be dy or dsum; dgamma and dbeta may be views whose workers lie apart."""
-        a = self._backward_args
+        a = self._mine.backward
         a.ld_s = self._rows(s, "s")
         a.ld_dy = self._rows(dy, "dy", s)
         rows = a.rows = s.numel() // self.cols
