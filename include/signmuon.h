@@ -385,7 +385,7 @@ int signmuon_momentum_norm_noalloc(const void* dev_grads, int32_t grad_dtype, co
  * The state buffer starts with the step number; it and everything else in the buffer is device data, so a step captured
  * in a CUDA graph counts on when it is replayed, and saving the state buffer saves the optimizer.
  * NaN and infinities in a gradient reach the entries they belong to (states in 8 bits: the block of 256 they belong to).
- * One context must not be used from two streams at once. */
+ * One context must not be used from two streams at once.  Its calls are made with the GPU of its buffers as the current one. */
 typedef struct signmuon_adamw signmuon_adamw;   /* opaque host object */
 
 typedef struct {
@@ -478,7 +478,8 @@ void signmuon_adamw_destroy(signmuon_adamw* ctx);
  * and the alignment fix: the same call gives the same bits.  Rows may lie apart (ld_*), entries of a row are neighbours.
  * Nothing is required of alignment beyond an entry's own; 16-byte aligned pointers and row distances are faster.
  * Several threads may use one bound context at once, but its backward passes share the workspace: one is called after the
- * other has returned, and on the same stream or ordered behind it. */
+ * other has returned, and on the same stream or ordered behind it.  Calls are made with the GPU of the arrays as the current
+ * one. */
 typedef struct signmuon_layernorm signmuon_layernorm;   /* opaque host object */
 
 typedef struct {
