@@ -403,7 +403,8 @@ typedef struct {
   int32_t num_workers;          /* M, 1..255: gradients that a step averages */
   int32_t state_bits;           /* 32 or 8 */
   int32_t flags;                /* SIGNMUON_ADAMW_FLAG_* */
-  double lr, beta_one, beta_two, eps;  /* betas in [0, 1), eps in [2^-120, 1] */
+  double lr, beta_one, beta_two, eps;  /* betas in [0, 1), eps in [2^-120, 1].  v is a float32: a g whose (1 - b2) g^2 is below
+                                          the least positive one, 2^-149, leaves v zero, and eps alone divides */
 } signmuon_adamw_config;
 
 /* MASTER: bf16 weights get a float32 copy in the state that the step works on; W is that copy rounded.  The first step

@@ -215,12 +215,14 @@ struct Factors {
   float step_size;       // lr / (1 - b1^t)
   float inv_root;        // 1 / sqrt(1 - b2^t)
   bool first;            // t == 1: master weights come from W
+  bool fast_roots;       // (8-bit states) roots_of will do beside this eps
 };
 
-// W's new value.  Root, reciprocal and product are approximate to 2^-22; eps is at least 2^-120, so nothing is denormal.
+// W's new value.  Root, reciprocal and product are approximate to 2^-22.  The second moment may be denormal (gradients of
+// 1e-18 and less) and still count beside a small eps; the denominator is at least eps, which is no less than 2^-120.
 __device__ __forceinline__ float root_of(float v) {
   float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
 __device__ __forceinline__ float inverse(float x) {
@@ -298,7 +300,10 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int lane, uint2 codes) {
 }
 // Correctly rounded roots of a pair in (2^-100, 2^120), and 0 of 0.  Newton's step for x^2 = v from an approximate root x:
 // the residual v - x^2 is exact in a fused multiply-add, and what the step leaves of the error (its square, 2^-44) decides
-// the last bit in one of 2^19 roots or fewer.  (Smaller v give some small value: 2^-126 is added where 0 would divide.)
+// the last bit in one of 2^19 roots or fewer.  (2^-126 is added where 0 would divide: smaller v lose digits, below 2^-117 more
+// than 2^-20 of the root, but never more than 2^-63.  The codes do not see that: such an entry is held as the least positive
+// number beside the block's largest, which is above 2^-60.  W's step does not either while that error over the root's correction
+// is at most 2^-23 of eps; for a smaller eps the roots are taken one by one.)
 __device__ __forceinline__ float_pair roots_of(float_pair v) {
   const float2 a = halves(pair_add(v, pair_of(0x1p-126f)));
   float y0, y1;
@@ -369,8 +374,7 @@ __device__ __forceinline__ float update_entries(Entries<N>& x, const Tensor& t, 
   }
   const float vt = largest<N, LANES, R>(r, lane);
   float rt;
-  if (__all_sync(0xffffffffu, vt > 0x1p-60f && vt < 0x1p120f)) {
-    // (roots of entries below 2^-100 are held as the least positive number, whatever they are)
+  if (f.fast_roots && __all_sync(0xffffffffu, vt > 0x1p-60f && vt < 0x1p120f)) {
     rt = halves(roots_of(pair_of(vt))).x;
 #pragma unroll
     for (int j = 0; j < N; ++j) r[j] = roots_of(r[j]);
@@ -671,7 +675,8 @@ __global__ void __launch_bounds__(THREADS, BITS == 8 ? 2 : 3) adamw_kernel(const
   wait_for_stream();
   Header* h = reinterpret_cast<Header*>(s.state);
   const float scale = s.scale ? __ldg(s.scale) : 1.f;
-  const Factors f = {scale * s.inv_workers, s.lr * __ldcg(&h->inv_correction), __ldcg(&h->inv_root_correction), __ldcg(&h->step) == 0};
+  const float inv_root = __ldcg(&h->inv_root_correction);
+  const Factors f = {scale * s.inv_workers, s.lr * __ldcg(&h->inv_correction), inv_root, __ldcg(&h->step) == 0, s.eps >= 0x1p-40f * inv_root};
   if (!(fabsf(scale) <= 3.402823466e38f)) return;       // not finite: the step is skipped, t does not advance
   constexpr int PASSES = passes_of(RING), TILE = SPAN * PASSES;
   const int lane = threadIdx.x & 31;
