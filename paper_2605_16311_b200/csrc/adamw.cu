@@ -79,6 +79,7 @@ struct Step {
   int32_t block_bytes;                           // room of a block in the ring
   float lr, b1, omb1, b2, omb2, eps, inv_workers;
   float minus_zero;                              // (product() below)
+  float fast_above;                              // (8-bit states) blocks whose largest v is above this take their roots from roots_of
   double beta_one, beta_two;
   int32_t advance;                               // the launch that ends the step
 };
@@ -215,7 +216,6 @@ struct Factors {
   float step_size;       // lr / (1 - b1^t)
   float inv_root;        // 1 / sqrt(1 - b2^t)
   bool first;            // t == 1: master weights come from W
-  bool fast_roots;       // (8-bit states) roots_of will do beside this eps
 };
 
 // W's new value.  Root, reciprocal and product are approximate to 2^-22.  The second moment may be denormal (gradients of
@@ -303,7 +303,8 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int lane, uint2 codes) {
 // the last bit in one of 2^19 roots or fewer.  (2^-126 is added where 0 would divide: smaller v lose digits, below 2^-117 more
 // than 2^-20 of the root, but never more than 2^-63.  The codes do not see that: such an entry is held as the least positive
 // number beside the block's largest, which is above 2^-60.  W's step does not either while that error over the root's correction
-// is at most 2^-23 of eps; for a smaller eps the roots are taken one by one.)
+// is at most 2^-23 of eps; for a smaller eps the roots are taken one by one: fast_above is infinite then.  It is a constant of the
+// launch because a flag in a register costs 2 % here, 320 us for 157 M entries and not 313.)
 __device__ __forceinline__ float_pair roots_of(float_pair v) {
   const float2 a = halves(pair_add(v, pair_of(0x1p-126f)));
   float y0, y1;
@@ -374,7 +375,7 @@ __device__ __forceinline__ float update_entries(Entries<N>& x, const Tensor& t, 
   }
   const float vt = largest<N, LANES, R>(r, lane);
   float rt;
-  if (f.fast_roots && __all_sync(0xffffffffu, vt > 0x1p-60f && vt < 0x1p120f)) {
+  if (__all_sync(0xffffffffu, vt > s.fast_above && vt < 0x1p120f)) {
     rt = halves(roots_of(pair_of(vt))).x;
 #pragma unroll
     for (int j = 0; j < N; ++j) r[j] = roots_of(r[j]);
@@ -675,8 +676,7 @@ __global__ void __launch_bounds__(THREADS, BITS == 8 ? 2 : 3) adamw_kernel(const
   wait_for_stream();
   Header* h = reinterpret_cast<Header*>(s.state);
   const float scale = s.scale ? __ldg(s.scale) : 1.f;
-  const float inv_root = __ldcg(&h->inv_root_correction);
-  const Factors f = {scale * s.inv_workers, s.lr * __ldcg(&h->inv_correction), inv_root, __ldcg(&h->step) == 0, s.eps >= 0x1p-40f * inv_root};
+  const Factors f = {scale * s.inv_workers, s.lr * __ldcg(&h->inv_correction), __ldcg(&h->inv_root_correction), __ldcg(&h->step) == 0};
   if (!(fabsf(scale) <= 3.402823466e38f)) return;       // not finite: the step is skipped, t does not advance
   constexpr int PASSES = passes_of(RING), TILE = SPAN * PASSES;
   const int lane = threadIdx.x & 31;
@@ -1104,6 +1104,7 @@ int signmuon_adamw_step(signmuon_adamw* c, void* const* weights, const void* con
   s.omb2 = (float)(1 - s.beta_two);
   s.eps = (float)c->cfg.eps;
   s.minus_zero = -0.f;
+  s.fast_above = c->cfg.eps >= 0x1p-40 / std::sqrt(1 - s.beta_two) ? 0x1p-60f : INFINITY;      // (the correction is largest at t = 1)
   s.inv_workers = (float)(1.0 / s.workers);
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (c->launches.size() > 1) {              // a pointer that is refused is refused before the first launch
