@@ -151,8 +151,10 @@ class AdamW:
             raise ValueError("no tensors given, and none attached")
         if lr is not None and not 0 <= lr < math.inf:
             raise ValueError(f"lr is {lr}")
-        code = B.on_device(self._index, self._lib.signmuon_adamw_step, self.ctx, w, g, -1.0 if lr is None else lr,
-                           None if scale is None else self._scalar(scale), _stream(self._index))
+        call = self._lib.signmuon_adamw_step
+        if B._current_device() != self._index:
+            call = B.on_device(self._index, call)
+        code = call(self.ctx, w, g, -1.0 if lr is None else lr, None if scale is None else self._scalar(scale), _stream(self._index))
         if code:
             raise B.SignMuonError(code, "signmuon_adamw_step")
 
@@ -166,7 +168,10 @@ class AdamW:
             out = torch.empty_like(self._two)
         elif out.dtype != torch.float32 or out.device != self.device or out.numel() != 2 or not out.is_contiguous():
             raise ValueError("out is two float32 on the optimizer's device")
-        code = B.on_device(self._index, self._lib.signmuon_adamw_grad_norm, self.ctx, g, max_norm, out.data_ptr(), _stream(self._index))
+        call = self._lib.signmuon_adamw_grad_norm
+        if B._current_device() != self._index:
+            call = B.on_device(self._index, call)
+        code = call(self.ctx, g, max_norm, out.data_ptr(), _stream(self._index))
         if code:
             raise B.SignMuonError(code, "signmuon_adamw_grad_norm")
         return out

@@ -420,13 +420,13 @@ def cuda_device(device) -> torch.device:
 _current_device = torch._C._cuda_getDevice       # (torch.cuda.current_device costs three times as much)
 
 
-def on_device(index: int, call, *args):
-    """call(*args) with GPU `index` as the current one.  The library launches on the current GPU, whatever GPU the pointers
-    belong to, and the default stream has the same handle on every GPU."""
-    if _current_device() == index:
-        return call(*args)
-    with torch.cuda.device(index):
-        return call(*args)
+def on_device(index: int, call):
+    """The call with GPU `index` as the current one.  The library launches on the current GPU, whatever GPU the pointers belong
+    to, and the default stream has the same handle on every GPU."""
+    def switched(*args):
+        with torch.cuda.device(index):
+            return call(*args)
+    return switched
 
 
 _DT = {"f32": F32, "bf16": BF16}

@@ -121,7 +121,10 @@ class LayerNorm:
         else:
             a.mean = a.rstd = None
         a.x, a.y, a.gamma, a.beta = x.data_ptr(), y.data_ptr(), self._weight(gamma, "gamma"), self._weight(beta, "beta")
-        code = B.on_device(self._index, self._lib.signmuon_layernorm_forward, self.ctx, C.byref(a), _stream(self._index))
+        call = self._lib.signmuon_layernorm_forward
+        if B._current_device() != self._index:
+            call = B.on_device(self._index, call)
+        code = call(self.ctx, C.byref(a), _stream(self._index))
         if code:
             raise B.SignMuonError(code, "signmuon_layernorm_forward")
         return y, mean, rstd, s
@@ -151,7 +154,10 @@ class LayerNorm:
             dbeta, a.dbeta, a.dbeta_stride = self._gradient(dbeta, "dbeta")
         else:
             dbeta = a.dbeta = None
-        code = B.on_device(self._index, self._lib.signmuon_layernorm_backward, self.ctx, C.byref(a), _stream(self._index))
+        call = self._lib.signmuon_layernorm_backward
+        if B._current_device() != self._index:
+            call = B.on_device(self._index, call)
+        code = call(self.ctx, C.byref(a), _stream(self._index))
         if code:
             raise B.SignMuonError(code, "signmuon_layernorm_backward")
         return dx, dgamma, dbeta
