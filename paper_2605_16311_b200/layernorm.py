@@ -32,8 +32,9 @@ class _Arguments(threading.local):
 
 class LayerNorm:
     def __init__(self, cols: int, num_workers: int = 1, dtype: str = "bf16", weight_dtype: Optional[str] = None,
-                 grad_dtype: Optional[str] = None, eps: float = 1e-5, device: str = "cuda:0"):
-        self.cols, self.num_workers = cols, num_workers
+                 grad_dtype: Optional[str] = None, eps: float = 1e-5, device: str = "cuda:0", workspace: Optional[torch.Tensor] = None):
+        """`workspace`: that of another object of this width, whose backward passes then count as this one's."""
+        self.cols, self.num_workers, self.eps = cols, num_workers, eps
         self.device = B.cuda_device(device)
         self._index = self.device.index
         self.ctx = None
@@ -44,7 +45,12 @@ class LayerNorm:
         self.dtype, self.weight_dtype, self.grad_dtype = (_TORCH[n] for n in names)
         self.ctx = B.signmuon_layernorm_create(cols, num_workers, *(B._DT[n] for n in names), eps)
         self._lib = B.load_library()
-        self.workspace = torch.empty(B.signmuon_layernorm_workspace_bytes(self.ctx), dtype=torch.uint8, device=self.device)
+        self._names, self._whole = names, None
+        self.workspace = workspace
+        if workspace is None:
+            self.workspace = torch.empty(B.signmuon_layernorm_workspace_bytes(self.ctx), dtype=torch.uint8, device=self.device)
+        elif workspace.dtype != torch.uint8 or workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace is not bytes on {self.device}")
         with torch.cuda.device(self.device):
             B._check(self._lib.signmuon_layernorm_bind(self.ctx, self.workspace.data_ptr(), self.workspace.numel(), _stream(self._index)),
                      "signmuon_layernorm_bind")
@@ -56,7 +62,7 @@ class LayerNorm:
     def close(self):
         if self.ctx:
             B.load_library().signmuon_layernorm_destroy(self.ctx)
-            self.ctx = None
+            self.ctx = self._whole = None
 
     def __del__(self):
         try:
@@ -172,9 +178,17 @@ class LayerNorm:
             raise ValueError(f"{name}: the entries of a worker are not neighbours, or the workers overlap")
         return t, t.data_ptr(), t.stride(0) if self.num_workers > 1 else self.cols
 
+    def _of_all_workers(self) -> "LayerNorm":
+        """This norm with all rows those of one worker: its weight gradients are the sums over the workers."""
+        if self.num_workers == 1:
+            return self
+        if self._whole is None:
+            self._whole = LayerNorm(self.cols, 1, *self._names, self.eps, self.device, self.workspace)
+        return self._whole
+
     def apply(self, x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None):
         """y, or (y, x + residual), for torch's autograd.  gamma and beta are [cols] (their gradient is then the sum over
-        the workers) or [num_workers, cols] views expanded from one row, which receive every worker's own.  There are no
+        the workers, rounded once) or [num_workers, cols] views expanded from one row, which receive every worker's own.  There are no
         second derivatives: asking for one raises."""
         y, s = _Function.apply(self, x, gamma, beta, residual)
         return y if residual is None else (y, s)
@@ -205,12 +219,15 @@ class _Function(torch.autograd.Function):
 
 
 def _gradients(ln, apart, bias, dy, ds, s, gamma, mean, rstd):
-    dx, dgamma, dbeta = ln.backward(dy.contiguous(), s, gamma[0] if apart[0] else gamma, mean, rstd,
-                                    dsum=None if ds is None else ds.contiguous(), bias=bias)
-    dgamma = dgamma if apart[0] else dgamma.float().sum(0).to(dgamma.dtype)
-    if bias and not apart[1]:
-        dbeta = dbeta.float().sum(0).to(dbeta.dtype)
-    return dx, dgamma, dbeta
+    args = (dy.contiguous(), s, gamma[0] if apart[0] else gamma, mean, rstd, None if ds is None else ds.contiguous(), bias)
+    if apart[0]:
+        dx, dgamma, dbeta = ln.backward(*args)
+    else:
+        dx, dgamma, dbeta = ln._of_all_workers().backward(*args)
+        dgamma = dgamma[0]
+    if bias and apart[1] != apart[0]:       # one weight a worker's own, the other shared: a pass for each
+        dbeta = (ln if apart[1] else ln._of_all_workers()).backward(*args)[2]
+    return dx, dgamma, dbeta[0] if bias and not apart[1] else dbeta
 
 
 class _Backward(torch.autograd.Function):
