@@ -299,12 +299,12 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int lane, uint2 codes) {
   }
 }
 // Correctly rounded roots of a pair in (2^-100, 2^120), and 0 of 0.  Newton's step for x^2 = v from an approximate root x:
-// the residual v - x^2 is exact in a fused multiply-add, and what the step leaves of the error (its square, 2^-44) decides
-// the last bit in one of 2^19 roots or fewer.  (2^-126 is added where 0 would divide: smaller v lose digits, below 2^-117 more
-// than 2^-20 of the root, but never more than 2^-63.  The codes do not see that: such an entry is held as the least positive
-// number beside the block's largest, which is above 2^-60.  W's step does not either while that error over the root's correction
-// is at most 2^-23 of eps; for a smaller eps the roots are taken one by one: fast_above is infinite then.  It is a constant of the
-// launch because a flag in a register costs 2 % here, 320 us for 157 M entries and not 313.)
+// the residual v - x^2 is exact in a fused multiply-add, and what the step leaves of the error, its square, never decides the
+// last bit: every float32 in the range was compared with __fsqrt_rn on a B200.  (2^-126 is added where 0 would divide: smaller
+// v lose digits, below 2^-117 more than 2^-20 of the root, but never more than 2^-63.  The codes do not see that: such an entry
+// is held as the least positive number beside the block's largest, which is above 2^-60.  W's step does not either while that
+// error over the root's correction is at most 2^-23 of eps; for a smaller eps the roots are taken one by one: fast_above is
+// infinite then.  It is a constant of the launch: a flag in a register took 320 us for 157 M entries, this 309 us.)
 __device__ __forceinline__ float_pair roots_of(float_pair v) {
   const float2 a = halves(pair_add(v, pair_of(0x1p-126f)));
   float y0, y1;
