@@ -186,9 +186,9 @@ class LayerNorm:
             self._whole = LayerNorm(self.cols, 1, *self._names, self.eps, self.device, self.workspace)
         return self._whole
 
-    def apply(self, x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None):
+    def apply(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None):
         """y, or (y, x + residual), for torch's autograd.  gamma and beta are [cols] (their gradient is then the sum over
-        the workers, rounded once) or [num_workers, cols] views expanded from one row, which receive every worker's own.  There are no
+        the workers, rounded once) or None (ones, zeros), or [num_workers, cols] views expanded from one row, which receive every worker's own.  There are no
         second derivatives: asking for one raises."""
         y, s = _Function.apply(self, x, gamma, beta, residual)
         return y if residual is None else (y, s)
@@ -203,7 +203,8 @@ class _Function(torch.autograd.Function):
         one = [w[0] if w is not None and w.dim() == 2 else w for w in (gamma, beta)]
         y, mean, rstd, s = ln.forward(x, *one, residual=residual)
         fn.save_for_backward(s, gamma, mean, rstd)
-        fn.ln, fn.apart, fn.has = ln, [w is not None and w.dim() == 2 for w in (gamma, beta)], (beta is not None, residual is not None)
+        fn.ln, fn.apart = ln, [w is not None and w.dim() == 2 for w in (beta if gamma is None else gamma, beta)]
+        fn.has = (gamma is not None, beta is not None, residual is not None)
         if residual is None:
             fn.mark_non_differentiable(total := s.new_empty(0))
             return y, total
@@ -211,15 +212,15 @@ class _Function(torch.autograd.Function):
 
     @staticmethod
     def backward(fn, dy, ds):
-        bias, residual = fn.has
+        scaled, bias, residual = fn.has
         # (with create_graph as a function of its inputs, so that whoever differentiates it meets the refusal)
         call = _Backward.apply if torch.is_grad_enabled() else _gradients
         dx, dgamma, dbeta = call(fn.ln, fn.apart, bias, dy, ds if residual else None, *fn.saved_tensors)
-        return None, dx, dgamma, dbeta, dx if residual else None
+        return None, dx, dgamma if scaled else None, dbeta, dx if residual else None
 
 
 def _gradients(ln, apart, bias, dy, ds, s, gamma, mean, rstd):
-    args = (dy.contiguous(), s, gamma[0] if apart[0] else gamma, mean, rstd, None if ds is None else ds.contiguous(), bias)
+    args = (dy.contiguous(), s, gamma[0] if gamma is not None and gamma.dim() == 2 else gamma, mean, rstd, None if ds is None else ds.contiguous(), bias)
     if apart[0]:
         dx, dgamma, dbeta = ln.backward(*args)
     else:
