@@ -675,7 +675,7 @@ template <int BITS, bool MASTER, int RING, int CAP>
 __global__ void __launch_bounds__(THREADS, BITS == 8 ? 2 : 3) adamw_kernel(const __grid_constant__ Table<CAP> tab, const __grid_constant__ Step s) {
   wait_for_stream();
   Header* h = reinterpret_cast<Header*>(s.state);
-  const float scale = s.scale ? __ldg(s.scale) : 1.f;
+  const float scale = s.scale ? __ldcg(s.scale) : 1.f;      // (not __ldg: the kernel before this one may write it while this one runs)
   const Factors f = {scale * s.inv_workers, s.lr * __ldcg(&h->inv_correction), __ldcg(&h->inv_root_correction), __ldcg(&h->step) == 0};
   if (!(fabsf(scale) <= 3.402823466e38f)) return;       // not finite: the step is skipped, t does not advance
   constexpr int PASSES = passes_of(RING), TILE = SPAN * PASSES;
