@@ -132,9 +132,9 @@ class AdamW:
     def attach(self, weights, grads):
         """Names the tensors of the steps to come (weights None: of norms only), which have to stay where they are.  step()
         and grad_norm() without tensors take these; the checks and the pointers' table are done here, once."""
-        self._weights = None if weights is None else self._pointers(weights, False)
-        self._grads = self._pointers(grads, True)
-        self._kept = (weights, grads)
+        w, g = None if weights is None else self._pointers(weights, False), self._pointers(grads, True)
+        self._weights, self._grads = w, g
+        self._kept = (None if weights is None else tuple(weights), tuple(grads))      # (the caller's lists may change)
 
     def _scalar(self, t: torch.Tensor):
         if t.dtype != torch.float32 or t.device != self.device or t.numel() != 1:
