@@ -62,7 +62,12 @@ class AdamW:
 
     # ---- buffers
     def rebind(self, zero_state: bool = True):
-        """Binds the buffers again: clears the state, or (zero_state False) goes on with what `state` holds."""
+        """Binds the buffers again: clears the state, or (zero_state False) goes on with what `state` holds, also where another
+        tensor has been put in its place; views taken before are of the old one then."""
+        for t in (self.state, self.workspace):
+            if t.dtype != torch.uint8 or t.device != self.device or not t.is_contiguous():
+                raise ValueError(f"state and workspace are bytes on {self.device}: got {t.dtype} on {t.device}")
+        self._views = {}
         with torch.cuda.device(self.device):
             B._check(self._lib.signmuon_adamw_bind(self.ctx, self.state.data_ptr(), self.state.numel(), self.workspace.data_ptr(),
                                                    self.workspace.numel(), int(zero_state), _stream(self._index)), "signmuon_adamw_bind")
