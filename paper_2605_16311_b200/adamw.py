@@ -57,7 +57,7 @@ class AdamW:
         self.state = torch.empty(state_bytes, dtype=torch.uint8, device=self.device)
         self.workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=self.device)
         self._weights = self._grads = self._kept = None
-        self._views, self._two = {}, torch.empty(2, dtype=torch.float32, device=self.device)
+        self._streams, self._views, self._two = set(), {}, torch.empty(2, dtype=torch.float32, device=self.device)
         self.rebind()
 
     # ---- buffers
@@ -67,10 +67,18 @@ class AdamW:
         for t in (self.state, self.workspace):
             if t.dtype != torch.uint8 or t.device != self.device or not t.is_contiguous():
                 raise ValueError(f"state and workspace are bytes on {self.device}: got {t.dtype} on {t.device}")
-        self._views = {}
+        self._views, stream = {}, _stream(self._index)
+        self._streams = set()
+        self._meet(stream)
         with torch.cuda.device(self.device):
             B._check(self._lib.signmuon_adamw_bind(self.ctx, self.state.data_ptr(), self.state.numel(), self.workspace.data_ptr(),
-                                                   self.workspace.numel(), int(zero_state), _stream(self._index)), "signmuon_adamw_bind")
+                                                   self.workspace.numel(), int(zero_state), stream), "signmuon_adamw_bind")
+
+    def _meet(self, stream: int):
+        """A stream that has not used the buffers yet: should they be freed, the allocator waits for what it runs by then."""
+        for t in (self.state, self.workspace):
+            t.record_stream(torch.cuda.current_stream(self.device))
+        self._streams.add(stream)
 
     def close(self):
         if self.ctx:
@@ -112,8 +120,11 @@ class AdamW:
 
     def set_step(self, steps: int):
         """For states that were filled in from elsewhere: the number of steps behind them."""
+        stream = _stream(self._index)
+        if stream not in self._streams:
+            self._meet(stream)
         with torch.cuda.device(self.device):
-            B._check(self._lib.signmuon_adamw_set_step(self.ctx, steps, _stream(self._index)), "signmuon_adamw_set_step")
+            B._check(self._lib.signmuon_adamw_set_step(self.ctx, steps, stream), "signmuon_adamw_set_step")
 
     # ---- tensors
     def _pointers(self, tensors, grads: bool):
@@ -156,10 +167,13 @@ class AdamW:
             raise ValueError("no tensors given, and none attached")
         if lr is not None and not 0 <= lr < math.inf:
             raise ValueError(f"lr is {lr}")
+        stream = _stream(self._index)
+        if stream not in self._streams:
+            self._meet(stream)
         call = self._lib.signmuon_adamw_step
         if B._current_device() != self._index:
             call = B.on_device(self._index, call)
-        code = call(self.ctx, w, g, -1.0 if lr is None else lr, None if scale is None else self._scalar(scale), _stream(self._index))
+        code = call(self.ctx, w, g, -1.0 if lr is None else lr, None if scale is None else self._scalar(scale), stream)
         if code:
             raise B.SignMuonError(code, "signmuon_adamw_step")
 
@@ -173,10 +187,13 @@ class AdamW:
             out = torch.empty_like(self._two)
         elif out.dtype != torch.float32 or out.device != self.device or out.numel() != 2 or not out.is_contiguous():
             raise ValueError("out is two float32 on the optimizer's device")
+        stream = _stream(self._index)
+        if stream not in self._streams:
+            self._meet(stream)
         call = self._lib.signmuon_adamw_grad_norm
         if B._current_device() != self._index:
             call = B.on_device(self._index, call)
-        code = call(self.ctx, g, max_norm, out.data_ptr(), _stream(self._index))
+        code = call(self.ctx, g, max_norm, out.data_ptr(), stream)
         if code:
             raise B.SignMuonError(code, "signmuon_adamw_grad_norm")
         return out

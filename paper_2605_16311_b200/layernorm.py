@@ -45,7 +45,7 @@ class LayerNorm:
         self.dtype, self.weight_dtype, self.grad_dtype = (_TORCH[n] for n in names)
         self.ctx = B.signmuon_layernorm_create(cols, num_workers, *(B._DT[n] for n in names), eps)
         self._lib = B.load_library()
-        self._names, self._whole = names, None
+        self._names, self._whole, self._streams = names, None, set()
         self.workspace = workspace
         if workspace is None:
             self.workspace = torch.empty(B.signmuon_layernorm_workspace_bytes(self.ctx), dtype=torch.uint8, device=self.device)
@@ -58,6 +58,11 @@ class LayerNorm:
         self._weight_gradient = torch.empty(1, dtype=self.grad_dtype, device=self.device).expand(num_workers, cols)
         self._one = torch.empty(1, dtype=torch.float32, device=self.device)
         self._mine = _Arguments(self._one)
+
+    def _meet(self, stream: int):
+        """A stream that has not used the workspace yet: should it be freed, the allocator waits for what that one runs by then."""
+        self.workspace.record_stream(torch.cuda.current_stream(self.device))
+        self._streams.add(stream)
 
     def close(self):
         if self.ctx:
@@ -160,10 +165,13 @@ class LayerNorm:
             dbeta, a.dbeta, a.dbeta_stride = self._gradient(dbeta, "dbeta")
         else:
             dbeta = a.dbeta = None
+        stream = _stream(self._index)
+        if stream not in self._streams:
+            self._meet(stream)
         call = self._lib.signmuon_layernorm_backward
         if B._current_device() != self._index:
             call = B.on_device(self._index, call)
-        code = call(self.ctx, C.byref(a), _stream(self._index))
+        code = call(self.ctx, C.byref(a), stream)
         if code:
             raise B.SignMuonError(code, "signmuon_layernorm_backward")
         return dx, dgamma, dbeta
