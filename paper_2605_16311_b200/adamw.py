@@ -45,6 +45,7 @@ class AdamW:
         self.num_workers, self.state_bits, self.lr = num_workers, state_bits, lr
         self.device = B.cuda_device(device)
         self._index = self.device.index
+        self._alone = torch.cuda.device_count() == 1       # (the only GPU is always the current one)
         self.ctx = None
         for p in self.params:
             if p.dtype not in _TORCH or p.grad_dtype not in _TORCH:
@@ -171,7 +172,7 @@ class AdamW:
         if stream not in self._streams:
             self._meet(stream)
         call = self._lib.signmuon_adamw_step
-        if B._current_device() != self._index:
+        if not self._alone and B._current_device() != self._index:
             call = B.on_device(self._index, call)
         code = call(self.ctx, w, g, -1.0 if lr is None else lr, None if scale is None else self._scalar(scale), stream)
         if code:
@@ -191,7 +192,7 @@ class AdamW:
         if stream not in self._streams:
             self._meet(stream)
         call = self._lib.signmuon_adamw_grad_norm
-        if B._current_device() != self._index:
+        if not self._alone and B._current_device() != self._index:
             call = B.on_device(self._index, call)
         code = call(self.ctx, g, max_norm, out.data_ptr(), stream)
         if code:

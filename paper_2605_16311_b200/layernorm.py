@@ -37,6 +37,7 @@ class LayerNorm:
         self.cols, self.num_workers, self.eps = cols, num_workers, eps
         self.device = B.cuda_device(device)
         self._index = self.device.index
+        self._alone = torch.cuda.device_count() == 1       # (the only GPU is always the current one)
         self.ctx = None
         names = (dtype, weight_dtype or dtype, grad_dtype or weight_dtype or dtype)
         for n in names:
@@ -133,7 +134,7 @@ class LayerNorm:
             a.mean = a.rstd = None
         a.x, a.y, a.gamma, a.beta = x.data_ptr(), y.data_ptr(), self._weight(gamma, "gamma"), self._weight(beta, "beta")
         call = self._lib.signmuon_layernorm_forward
-        if B._current_device() != self._index:
+        if not self._alone and B._current_device() != self._index:
             call = B.on_device(self._index, call)
         code = call(self.ctx, C.byref(a), _stream(self._index))
         if code:
@@ -169,7 +170,7 @@ class LayerNorm:
         if stream not in self._streams:
             self._meet(stream)
         call = self._lib.signmuon_layernorm_backward
-        if B._current_device() != self._index:
+        if not self._alone and B._current_device() != self._index:
             call = B.on_device(self._index, call)
         code = call(self.ctx, C.byref(a), stream)
         if code:
