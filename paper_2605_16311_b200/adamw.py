@@ -160,7 +160,9 @@ class AdamW:
 
     def step(self, weights=None, grads=None, lr: Optional[float] = None, scale: Optional[torch.Tensor] = None):
         """One step on the current stream.  `scale`: device float32 that multiplies the mean gradient (a clip coefficient, an
-        inverse loss scale); when it is not finite the device skips the step."""
+        inverse loss scale); when it is not finite the device skips the step.  Tensors that are given are checked every time, about
+        1.3 us each on the host; attached ones are not.  The weights change behind autograd's back: a backward pass of a graph
+        that saved them has to come before."""
         if (weights is None) != (grads is None):
             raise ValueError("step takes weights and gradients, or neither")
         w, g = (self._weights, self._grads) if weights is None else (self._pointers(weights, False), self._pointers(grads, True))

@@ -666,10 +666,13 @@ __device__ __noinline__ void update_rest(const Tensor& t, const Step& s, const F
 // - 32 bits: the memory.  25.5 M float32 entries with 4 workers (1.02 GB): 159 us, 6.4 TB/s; 39.4 M bf16 entries with master
 //   weights (1.10 GB): 176 us, 6.3 TB/s.  Three thread blocks an SM keep 72 to 96 KB in flight; with two the latter takes 201
 //   us, with four 186 us.
-// - 8 bits: bf16, the issue of instructions, about 40 an entry for its 10 bytes.  157 M entries (1.58 GB): 273 us in a short
-//   run, 5.8 TB/s; 297 us where the clock has fallen under a long one.  The root and the separate roundings of the exact codes
-//   are a fifth of the work (252 us without, before the last steps; but then one code in 10^5 differs from the formula's).
-//   float32 weights or master copies: the memory (39.4 M entries: 107 and 105 us, 5.9 and 6.1 TB/s).
+// - 8 bits: bf16, the issue of instructions, about 40 an entry for its 10 bytes.  157 M entries (1.58 GB): 309 us, 5.1 TB/s
+//   (273 us in a run so short that the clock stays high).  The root and the separate roundings of the exact codes are a fifth of
+//   the work (252 us without, before the last steps; but then one code in 10^5 differs from the formula's).
+//   float32 weights: the memory (39.4 M entries with one worker: 103 us, 6.2 TB/s).
+// - 8 bits without the ring, large sets (two float32 gradients beside float32 weights or master copies, five bf16 gradients and
+//   more): the latency of a block's loads, with nothing of the warp in flight beside them.  39.4 M entries take 188 us with two
+//   float32 gradients (4.2 TB/s), 185 us with five and with eight bf16 ones (3.8 and 5.1 TB/s), 267 us with 16 (5.9 TB/s).
 // - small sets: latency.  19 k entries of 25 tensors with 16 workers: 3.4 us a step, launched back to back.
 template <int BITS, bool MASTER, int RING, int CAP>
 __global__ void __launch_bounds__(THREADS, BITS == 8 ? 2 : 3) adamw_kernel(const __grid_constant__ Table<CAP> tab, const __grid_constant__ Step s) {

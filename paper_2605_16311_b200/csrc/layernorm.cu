@@ -635,8 +635,9 @@ template <typename AT, int T, int E> struct BackwardRing {
 
 // As backward_kernel, with the rows to come in flight through shared memory.  Every thread keeps the sums of its columns in
 // registers (2 E of them), which leaves 12 to 16 warps an SM: too few to hide a row's two sums behind other rows entirely.
-// 16384 x 768 bf16 with dsum (101 MB): 22.4 us with the joining kernel, 4.5 TB/s; 16384 x 4096 (403 MB): 73.7 us, 5.5 TB/s.  Several groups share a thread block so that one leaves a single row of partial sums (1024 columns: 48 us with
-// 64 threads a block, 39 us so).
+// 16384 x 768 bf16 with dsum (101 MB): 22.5 us with the joining kernel, 4.5 TB/s; 16384 x 4096 (403 MB): 77.4 us, 5.2 TB/s.
+// Several groups share a thread block so that one leaves a single row of partial sums (1024 columns: 48 us with 64 threads a
+// block, 39 us so).
 template <typename AT, int T, int E>
 __global__ void __launch_bounds__(BackwardRing<AT, T, E>::NT, BackwardRing<AT, T, E>::BLOCKS) backward_ring_kernel(const Backward a) {
   using R = BackwardRing<AT, T, E>;
@@ -1169,7 +1170,9 @@ int signmuon_layernorm_backward(signmuon_layernorm* c, const signmuon_layernorm_
   const Choice f = half ? (vec ? choose_backward<bf16, true>(cols, arrays) : choose_backward<bf16, false>(cols, arrays))
                         : (vec ? choose_backward<float, true>(cols, arrays) : choose_backward<float, false>(cols, arrays));
   const bool weights = q.dgamma || q.dbeta;
-  // one wave of thread blocks, every group with a row at least; the columns' kernel shares a row out over several
+  // One wave of thread blocks, every group with a row at least; the columns' kernel shares a row out over several.  Where the
+  // workers do not divide the wave, the SMs that are left over have nothing to do, and from half a wave on there is one thread
+  // block a worker: 14.8 k rows of 768 take 19.1 us for 64 workers, 21.4 us for 75, 18.4 us for 100, 17.2 us for 148.
   const int64_t across = COLUMN_THREADS * (vec ? unit : 1), side = (cols + across - 1) / across;
   const int blocks = f.wide ? 8 : c->resident(f, !vec ? c->BACKWARD_SINGLE : q.dsum ? c->BACKWARD_DSUM : c->BACKWARD);
   const int64_t target = std::min<int64_t>(c->max_parts, f.wide ? (c->sms * 8 + side - 1) / side : (int64_t)c->sms * blocks);

@@ -109,7 +109,8 @@ class LayerNorm:
     def forward(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
                 residual: Optional[torch.Tensor] = None, stats: bool = True, out: Optional[torch.Tensor] = None):
         """(y, mean, rstd, s).  s is x + residual, or x itself without one; mean and rstd are None without `stats`.
-        gamma None: ones, beta None: zeros.  `out` takes y, and may be x."""
+        gamma None: ones, beta None: zeros.  `out` takes y, and may be x (without a residual, s is then what y has become: no
+        backward pass can follow)."""
         mine = self._mine
         a = mine.forward
         a.ld_x = self._rows(x, "x")
