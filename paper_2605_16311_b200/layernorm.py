@@ -198,8 +198,8 @@ class LayerNorm:
 
     def apply(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None):
         """y, or (y, x + residual), for torch's autograd.  gamma and beta are [cols] (their gradient is then the sum over
-        the workers, rounded once) or None (ones, zeros), or [num_workers, cols] views expanded from one row, which receive every worker's own.  There are no
-        second derivatives: asking for one raises."""
+        the workers, rounded once), or [num_workers, cols] views expanded from one row, which receive every worker's own, or
+        None (ones, zeros).  There are no second derivatives: asking for one raises."""
         y, s = _Function.apply(self, x, gamma, beta, residual)
         return y if residual is None else (y, s)
 
